@@ -673,7 +673,9 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
         m0 = lane < 8 ? ma : mb;
         l0 = lane < 8 ? la : lb;
       }
-      // (the place of the maxima two steps ago)
+      // The place of the maxima two steps ago, which both have read: they met in the last step.  Not so where the second of two halves of rows has none for
+      // these warps, which pass its steps without meeting.
+      if (seg.dual) ok = both() && ok;
       auto other = [&](float x) {
         sh.half[step & 1][half][r] = x;
         ok = both() && ok;
