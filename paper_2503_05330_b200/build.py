@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libsdms.so")
 OBJECTS = os.path.join(HERE, "_build")
 SOURCES = ["api.cu", "append.cu", "match.cu", "dag.cu", "dag_wide.cu", "beams.cu", "fuzzy.cu", "match_static.cu",
            "decode_api.cu", "kv.cu", "beam_select.cu", "attend.cu"]
-HEADERS = ["sdms_dev.cuh", "sdms_internal.h", "append_dev.cuh", "wide_dev.cuh", "beam_dev.cuh", "beam_plan.h", "decode_internal.h", "decode_dev.cuh"]
+HEADERS = ["sdms_dev.cuh", "sdms_internal.h", "append_dev.cuh", "wide_dev.cuh", "beam_dev.cuh", "beam_plan.h", "decode_internal.h", "decode_dev.cuh", "attend_plan.h"]
 
 
 def _newest(files) -> float:

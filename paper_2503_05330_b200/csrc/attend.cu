@@ -20,6 +20,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include "attend_plan.h"
 #include "decode_dev.cuh"
 
 namespace sdms {
@@ -27,7 +28,6 @@ namespace sdms {
 namespace {
 
 constexpr int kTile = 128;               // keys of a tile, rows of a product
-constexpr int kCtas = 148;
 constexpr int kBlock = 64 * kTile * 2;   // a tile's 64 columns: 128 rows of 128 bytes, swizzled
 constexpr float kLazy = 8.f;             // a row's reference may lag behind its maximum by 2^8 before its sums are scaled anew
 constexpr int kUnit = 64;                // keys of a tile that one softmax thread has
@@ -1118,9 +1118,10 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const AttendD
   const int2 c_pre = parts.range[i_pre], c_own = parts.range[plan.pre_items + i_own];
   const int keys_pre = keys_of(a, g), keys_own = keys_of(a, a.G + p);
   if (t >= queries_of(a, p)) return;
-  const int n_pre = keys_pre ? c_pre.y - c_pre.x + 1 : 0, n_own = keys_own ? c_own.y - c_own.x + 1 : 0, parts_n = n_pre + n_own;
-  const long long first_pre = part_row(plan, true, i_pre, c_pre.x) + r_pre % (2 * kTile);
-  const long long first_own = part_row(plan, false, i_own, c_own.x) + r_own % (2 * kTile);
+  const PartRun pre = part_run(c_pre.x, c_pre.y), own = part_run(c_own.x, c_own.y);
+  const int n_pre = keys_pre ? pre.count : 0, n_own = keys_own ? own.count : 0, parts_n = n_pre + n_own;
+  const long long first_pre = part_row(plan, true, i_pre, pre.first) + r_pre % (2 * kTile);
+  const long long first_own = part_row(plan, false, i_own, own.first) + r_own % (2 * kTile);
   auto row_of = [&](int i) { return i < n_pre ? first_pre + (long long)i * plan.pre_slot : first_own + (long long)(i - n_pre) * plan.own_slot; };
   // Eight parts at a time, sums, references and totals under way together (18 parts a row: 7.3 us; four at a time, behind their references, 10.7;
   // sixteen 6.7, but 11.5 for 9.0 where rows have two or three).
