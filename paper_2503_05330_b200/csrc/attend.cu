@@ -752,9 +752,6 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
         if (++slot == kRing) { slot = 0; phase ^= 1; }
         return true;
       });
-    // (given up: what was asked for arrives before the shared memory is given back, or a millisecond has passed)
-    if (!ok)
-      for (const long long begin = clock64(); clock64() - begin < 2000000;) {}
   } else if (warp == 9) {
     // ---- products ----
     int slot = 0;
@@ -1089,6 +1086,10 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
   __syncwarp();
   fence_before();
   __syncthreads();
+  // Given up, whichever warp it was: tiles and products that are under way, asked for by warps that came to their own end, arrive before memory is given back, or a
+  // millisecond has passed.  (Nobody asks for any behind the barrier.)
+  if (dead)
+    for (const long long begin = clock64(); clock64() - begin < 2000000;) {}
   if (warp == 9) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tensor), "r"(kTensorColumns) : "memory");

@@ -43,3 +43,13 @@ def test_the_join_goes_by_them():
     for name in ("c_pre", "c_own"):
         rest = join.replace(f"{name} = parts.range", "").replace(f"part_run({name}.x, {name}.y)", "")
         assert f"{name}.x" not in rest and f"{name}.y" not in rest
+
+
+def test_who_gives_up_waits_for_what_is_under_way():
+    """Where any warp has given up, all wait between the CTA's last barrier and its end, so that no tile is written to shared memory that is another's by then."""
+    with open(os.path.join(CSRC, "attend.cu")) as f:
+        kernel = f.read().split("\nattend_kernel(", 1)[1].split("attend_join_kernel(const AttendDev a) {", 1)[0]
+    end = kernel.rsplit("__syncthreads();", 1)[1]
+    wait, rest = end.split("tcgen05.dealloc", 1)
+    assert "if (dead)" in wait and "clock64() - begin <" in wait
+    assert "clock64()" not in rest
