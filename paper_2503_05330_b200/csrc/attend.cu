@@ -897,7 +897,8 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
   } else if (warp < 10 + S::kConverters) {
     // ---- 8 bits to 16 ----
     // A code's seven bits of exponent and mantissa are a bfloat16's but for the exponent's offset: code << 4 reads as value * 2^-120, subnormal codes
-    // included, and one multiplication by a power of two sets that right and applies the token's scale.  Exact.  A warp has 16 tokens of a tile.
+    // included, and one multiplication by a power of two sets that right and applies the token's scale.  Exact, but for the two codes that are not numbers,
+    // which are looked for on the way and put right behind it (16 x 9 tokens: 75.5 us for 73.5 without a look).  A warp has 16 tokens of a tile.
     constexpr int kTokens = kTile / (S::kConverters ? S::kConverters : 1), kPieces = D / 16;
     const int token0 = (warp - 10) * kTokens;
     int slot = 0, raw = 0;
@@ -925,16 +926,19 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
         if (!__all_sync(~0u, bar_wait(&bars.raw_full[raw], phase_raw, &dead) && bar_wait(&bars.empty[slot], phase, &dead))) return false;
         const unsigned char* from = sm_raw + raw * S::kRaw + (token0 + my_token) * D + my_piece * 16;
         unsigned char* to = sm_kv + slot * S::kOperand + (my_piece >> 2) * kBlock + (token0 + my_token) * 128;
+        uint32_t most = 0;                                          // of the codes without their signs, one in each half
 #pragma unroll
         for (int x = 0; x < kTokens; x += kStep) {
           const uint4 w = *reinterpret_cast<const uint4*>(from + x * D);
           const uint32_t g1 = __shfl_sync(~0u, first, x + my_token);
           const uint32_t in[4] = {w.x, w.y, w.z, w.w};
-          uint32_t out[8];
+          uint32_t out[8], before = 0;
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const uint32_t t = __byte_perm(in[k >> 1], 0u, k & 1 ? 0x3424 : 0x1404);
-            const uint32_t b = (t & 0x80008000u) | (t >> 4 & 0x07f007f0u);
+            const uint32_t t = __byte_perm(in[k >> 1], 0u, k & 1 ? 0x3322 : 0x1100);
+            const uint32_t size = t << 4 & 0x07f007f0u, b = (t & 0x80008000u) | size;
+            if (k & 1) most = __vimax3_u16x2(most, size, before);
+            before = size;
             const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), *reinterpret_cast<const __nv_bfloat162*>(&g1));
             out[k] = *reinterpret_cast<const uint32_t*>(&y);
           }
@@ -950,6 +954,17 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
           const int c0 = (my_piece & 3) * 2, r = (my_token + x) & 7;                // (token0 is a multiple of eight)
           *reinterpret_cast<uint4*>(at + ((c0 ^ r) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
           *reinterpret_cast<uint4*>(at + (((c0 + 1) ^ r) << 4)) = make_uint4(out[4], out[5], out[6], out[7]);
+        }
+        // The code that is not a number, 0x7f, read as 480 above.  (Hardly ever there.)
+        if ((most + 0x00100010u) & 0x08000800u) {
+#pragma unroll 1
+          for (int i = 0; i < kTokens / kStep * 16; ++i) {
+            const int x = (i >> 4) * kStep, k = i & 15, t = token0 + my_token + x, key2 = j * kTile + t;
+            if ((from[x * D + k] & 0x7f) != 0x7f || key2 >= seg.keys) continue;
+            const bool note = v && key2 >= seg.whole && doubtful(seg);
+            *reinterpret_cast<uint16_t*>(to + x * 128 + ((((my_piece & 3) * 2 + (k >> 3)) ^ (t & 7)) << 4) + (k & 7) * 2) = note ? 0 : 0x7fc0;
+            if (note) atomicOr(&sh.unfinite[seg.place], 1ull << (key2 - seg.whole));
+          }
         }
         fence_async();
         __syncwarp();

@@ -31,3 +31,79 @@ def test_own_rows_that_leave_warps_without_one(kind, q_type):
         args[1].fill_(7.0)
         att(*args)
         assert torch.equal(args[1], first)
+
+
+def spoiled_attention(d, T, lens, prefix_len, spoil, mask=None, seed=90):
+    """8-bit caches that `spoil` has been at: (output, expected, tolerance)."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    P, group, heads = len(lens), 2, 2
+    paths = make_cache(P, 300, heads, d, torch.float8_e4m3fn, gen)
+    prefix = make_cache(1, 200, heads, d, torch.float8_e4m3fn, gen)
+    spoil(paths, prefix)
+    q = torch.randn((P, T, heads * group, d), device=DEV, generator=gen).to(torch.bfloat16)
+    out = torch.full_like(q, 7.0)
+    i32 = dict(device=DEV, dtype=torch.int32)
+    attention = binding.PathAttention(1, P, T, heads * group, heads, d, torch.bfloat16)
+    attention(q, out, paths, torch.tensor(lens, **i32), None, mask, prefix, torch.tensor([prefix_len], **i32))
+    assert not attention.timed_out()
+    expect, tol = ref.attend(q, ref.cache_values(paths.k, paths.k_scale), ref.cache_values(paths.v, paths.v_scale), lens, None, d ** -0.5,
+                             ref.cache_values(prefix.k, prefix.k_scale), ref.cache_values(prefix.v, prefix.v_scale), [prefix_len], mask)
+    return out, expect, tol
+
+
+@pytest.mark.parametrize("scale", [0, 120, 134, 135, 254])
+@pytest.mark.parametrize("code", [0x7f, 0xff])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("where", ["k", "v", "k_prefix", "v_prefix"])
+def test_codes_that_are_not_numbers(where, d, code, scale):
+    """float8_e4m3fn's own NaN, under whatever scale: in K no query that sees the key has an answer, in V one element has none."""
+    token, head, element = 77, 1, d - 3
+
+    def spoil(paths, prefix):
+        c, row = (prefix, 0) if "prefix" in where else (paths, 1)
+        x, s = (c.k, c.k_scale) if where[0] == "k" else (c.v, c.v_scale)
+        x.view(torch.uint8)[row, token, head, element] = code
+        if scale == 254:                                     # (the other elements of such a vector are zero: they are numbers that no sum holds)
+            x.view(torch.uint8)[row, token, head, :element] = 0
+            x.view(torch.uint8)[row, token, head, element + 1:] = 0
+        s[row, head, token] = scale
+    out, expect, tol = spoiled_attention(d, 1, [100, 130, 140], 199, spoil)
+    want = torch.isnan(expect)
+    rows = [0, 1, 2] if "prefix" in where else [1]
+    assert bool(want[rows, :, 2:, element].all()) and int(want.sum()) == len(rows) * 2 * (d if where[0] == "k" else 1)
+    assert torch.equal(torch.isnan(out), want)
+    assert bool(((out.double() - expect).abs() <= tol)[~want].all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T,tree", [(2, False), (9, False), (9, True), (64, False)])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_codes_that_are_not_numbers_in_new_tokens(where, T, tree, d):
+    """What a query does not see does it no harm; for those that see it nothing is left."""
+    lens = [0, 127, 128 - T // 2]
+    mask = None
+    if tree:
+        mask = torch.tensor([[1 << t | (t % 2) for t in range(T)]] * 3, device=DEV)
+
+    def spoil(paths, prefix):
+        c = paths.k if where == "k" else paths.v
+        for p, at in enumerate(lens):
+            for u, code in ((T - 1, 0x7f), (T // 2, 0xff)):
+                c.view(torch.uint8)[p, at + u, u % 2, (u * 11 + 5) % d] = code
+    out, expect, tol = spoiled_attention(d, T, lens, 150, spoil, mask)
+    reached = torch.isnan(expect).any(-1)
+    assert reached.any() and not reached.all()
+    assert bool(torch.isnan(out[reached]).all())
+    assert bool(((out.double() - expect).abs() <= tol)[~reached].all())
+
+
+def test_codes_that_are_not_numbers_behind_the_last_key():
+    def spoil(paths, prefix):
+        for p, n in enumerate((4, 133, 260)):
+            for x in (paths.k, paths.v):
+                x.view(torch.uint8)[p, n:] = 0x7f
+        for x in (prefix.k, prefix.v):
+            x.view(torch.uint8)[:, 100:] = 0xff
+    out, expect, tol = spoiled_attention(128, 3, [1, 130, 257], 100, spoil)
+    assert bool(torch.isfinite(expect).all()) and bool(((out.double() - expect).abs() <= tol).all())
