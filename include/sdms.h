@@ -399,7 +399,8 @@ int sdms_match_noalloc(const int32_t* d_tok, const int32_t* d_len, int32_t num_g
  * stride_head + i of d_k and d_v, so both [row][token][head][i] and [row][head][token][i] will do.  d_k and d_v
  * are 16-byte aligned and the strides multiples of 16 bytes (those of axes of length 1 are not looked at).
  * SDMS_TYPE_E4M3: what is stored times its token's and head's scale 2^(s - 127), s in d_k_scale / d_v_scale
- * [rows][heads][capacity] (s = 255: the vector reads as NaN).  Other types: those two are NULL.
+ * [rows][heads][capacity] (s = 255: the vector reads as NaN; so does the code 0x7f, with either sign, whatever the scale), rounded to
+ * bfloat16 where that is smaller than its normal numbers, and no larger than its largest.  Other types: those two are NULL.
  * SDMS_ERR_TOO_LARGE: more than 65535 rows, 1024 heads or 2^30 tokens of capacity.
  */
 typedef struct {

@@ -897,8 +897,9 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
   } else if (warp < 10 + S::kConverters) {
     // ---- 8 bits to 16 ----
     // A code's seven bits of exponent and mantissa are a bfloat16's but for the exponent's offset: code << 4 reads as value * 2^-120, subnormal codes
-    // included, and one multiplication by a power of two sets that right and applies the token's scale.  Exact, but for the two codes that are not numbers,
-    // which are looked for on the way and put right behind it (16 x 9 tokens: 75.5 us for 73.5 without a look).  A warp has 16 tokens of a tile.
+    // included, and one multiplication by a power of two sets that right and applies the token's scale.  Exact, but for values that a
+    // bfloat16 does not hold, and for the two codes that are not numbers, which are looked for on the way and put right behind it (16 x 9 tokens: 75.5 us
+    // for 73.5 without a look).  A warp has 16 tokens of a tile.
     constexpr int kTokens = kTile / (S::kConverters ? S::kConverters : 1), kPieces = D / 16;
     const int token0 = (warp - 10) * kTokens;
     int slot = 0, raw = 0;
@@ -954,6 +955,20 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
           const int c0 = (my_piece & 3) * 2, r = (my_token + x) & 7;                // (token0 is a multiple of eight)
           *reinterpret_cast<uint4*>(at + ((c0 ^ r) << 4)) = make_uint4(out[0], out[1], out[2], out[3]);
           *reinterpret_cast<uint4*>(at + (((c0 + 1) ^ r) << 4)) = make_uint4(out[4], out[5], out[6], out[7]);
+        }
+        // 256 * 2^120, which the largest bfloat16 is stored as, is none itself: what has become infinite is the largest number.  (NaN stays.  A loop of its own:
+        // in the one above the largest and smallest of two cost 1.5 us of 75 where no scale is large.)
+        if (large) {
+#pragma unroll 1
+          for (int x = 0; x < kTokens; x += kStep)
+#pragma unroll 1
+            for (int k = 0; k < 8; ++k) {
+              uint32_t* at = reinterpret_cast<uint32_t*>(to + x * 128 + ((((my_piece & 3) * 2 + (k >> 2)) ^ ((my_token + x) & 7)) << 4)) + (k & 3);
+              uint32_t y = *at;
+              if ((y & 0x7fffu) == 0x7f80u) y -= 1u;
+              if ((y & 0x7fff0000u) == 0x7f800000u) y -= 0x10000u;
+              *at = y;
+            }
         }
         // The code that is not a number, 0x7f, read as 480 above.  (Hardly ever there.)
         if ((most + 0x00100010u) & 0x08000800u) {
