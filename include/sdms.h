@@ -451,7 +451,7 @@ int sdms_kv_reorder(const sdms_kv* kv, const int32_t* d_parent, const int32_t* d
  * new token makes all elements of the queries that see it NaN (with T = 1 and no mask: those elements what they are) and touches no
  * other query; what lies behind the lengths may be anything.
  * Types: q, out and caches all BF16 or all FP16, or BF16 with E4M3 caches.  The products' sums, softmax and its statistics are
- * held in 32 bits; weights are rounded to the query's type for the second product.
+ * held in 32 bits; weights are rounded to the query's type for the second product (FP16: what is below 2^-31 of the largest counts as nothing there).
  * d_q and d_out are 16-byte aligned, their strides multiples of 8 elements (q: 0 too, queries that paths or tokens share); d_out may be d_q.
  * SDMS_ERR_TOO_LARGE: more than 65535 paths, 1024 query heads or 2^27 output rows, or caches whose capacities add up to more than 2^32 / 24 tiles
  * of 128 keys, times heads, times 128 rows that read them.

@@ -29,7 +29,12 @@ namespace {
 
 constexpr int kTile = 128;               // keys of a tile, rows of a product
 constexpr int kBlock = 64 * kTile * 2;   // a tile's 64 columns: 128 rows of 128 bytes, swizzled
-constexpr float kLazy = 8.f;             // a row's reference may lag behind its maximum by 2^8 before its sums are scaled anew
+// A row's reference may lag behind its maximum by 2^lazy before its sums are scaled anew, and the largest weight is 2^lift or so.  bfloat16 has weights of any
+// size.  fp16 has none below 2^-25, so many small ones would be lost that the total counts, and none from 2^16 on: with 6 and 6 those from 2^-31 of the
+// largest are there, and 2^4 are left above for the rounding of references, which products of 2^25 need.
+template <bool BF16> struct Weights {
+  static constexpr float kLazy = BF16 ? 8.f : 6.f, kLift = BF16 ? 0.f : 6.f;
+};
 constexpr int kUnit = 64;                // keys of a tile that one softmax thread has
 constexpr uint32_t kColS = 0, kColO = 256;   // tensor memory: two tiles of products, the weights over the first half of each; two sums behind them
 constexpr int kTensorColumns = 512;
@@ -423,6 +428,7 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
     const int half = warp >> 2, r = tid & 127;
     const uint32_t at_lanes = tensor + ((uint32_t)(warp & 3) << 21);            // 32 * (warp % 4) in the upper half of an address
     const float c = a.scale * 1.4426950408889634f;
+    constexpr float kLazy = Weights<BF16>::kLazy, kLift = Weights<BF16>::kLift;
     int step = 0;                                                   // tiles of products so far
     uint32_t phase_o = 0;                                           // a bit per sum
     int o_place = 0, q_place = 0, q_uses = 0, q_said = 0;
@@ -554,7 +560,7 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
                 tensor_store(at_o + k * 32, w);
               }
             }
-            const float ref = m == -INFINITY ? 0.f : m * c;
+            const float ref = m == -INFINITY ? 0.f : m * c - kLift;
             // (All 64 on the special function unit: sixteen of them by a polynomial instead, 6.5 instructions each, took 480 us where this takes 405,
             // 64 x 5 tokens behind 65536.)
             const Pair scale = Pair::of(c, c), minus_ref = Pair::of(-ref, -ref);
@@ -630,7 +636,7 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
                 tensor_store(at_o, w);
               }
             }
-            const float ref = m0 == -INFINITY ? 0.f : m0 * c, ref1 = m1 == -INFINITY ? 0.f : m1 * c;
+            const float ref = m0 == -INFINITY ? 0.f : m0 * c - kLift, ref1 = m1 == -INFINITY ? 0.f : m1 * c - kLift;
             uint32_t w[16];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
@@ -709,7 +715,7 @@ attend_kernel(const __grid_constant__ Maps maps, const AttendDev a) {
             float total = t ? total1 : total0;
             const uint64_t unfinite = *(volatile unsigned long long*)&sh.unfinite[seg.place];
             if (unfinite && unfinite & bits_of(row)) total = NAN;
-            parts.ml[at + row] = make_float2(m == -INFINITY ? -INFINITY : m * c, total);
+            parts.ml[at + row] = make_float2(m == -INFINITY ? -INFINITY : m * c - kLift, total);
           }
         }
         fence_before();

@@ -1,4 +1,6 @@
 """Attention at the ends of what its types hold."""
+import math
+
 import pytest
 import torch
 
@@ -56,3 +58,25 @@ def test_values_beyond_bfloat16_count_as_its_largest(code, scale, d):
     binding.PathAttention(1, 2, 1, 2, 1, d, torch.bfloat16)(q, out, paths, torch.tensor([100, 100], device=DEV, dtype=torch.int32))
     expect, tol = ref.attend(q, clamped(paths.k, paths.k_scale), clamped(paths.v, paths.v_scale), [100, 100], None, d ** -0.5)
     assert bool(torch.isfinite(out).all()) and bool(((out.double() - expect).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("T,group", [(1, 1), (1, 24), (5, 40)])
+def test_many_small_weights_behind_a_large_one(T, group):
+    """One key 18 ahead of 16000 others in fp16: each of those weighs 2^-26 of it, all of them together 2^-12."""
+    P, n, d, lead = 148, 16000, 64, 18.0
+    k = torch.zeros((P, n, 1, d), device=DEV, dtype=torch.float16)
+    v = torch.ones_like(k)
+    k[:, 0, 0, 0] = 12
+    v[:, 0] = 0
+    q = torch.zeros((P, T, group, d), device=DEV, dtype=torch.float16)
+    q[..., 0] = lead / 12 * 8
+    out = torch.empty_like(q)
+    attention = binding.PathAttention(1, P, T, group, 1, d, torch.float16)
+    mask = torch.zeros((P, T), device=DEV, dtype=torch.int64)      # the new tokens are not looked at
+    attention(q, out, binding.KvCache(k, v), torch.full((P,), n - T, device=DEV, dtype=torch.int32), None, mask, scale=0.125)
+    assert not attention.timed_out()
+    small = math.exp(-lead) * (n - T - 1)
+    expect = small / (1 + small)
+    # a weight is rounded to 2^-25 of what a 16-bit number can be here, 2^6 times the largest weight; the output to half a step; exponents by 2^-21
+    tol = (n - T - 1) * 2.0 ** -31 + expect * (2.0 ** -11 + 2.0 ** -20)
+    assert bool(((out.double() - expect).abs() <= tol).all()), (float(out.min()), float(out.max()), expect, tol)
