@@ -30,6 +30,7 @@ constexpr int kRowThreads = 256;
 constexpr int kRowList = 2048, kList = 2048;   // candidates listed by a CTA of the one kernel and the other
 static_assert((kRowList & (kRowList - 1)) == 0 && (kList & (kList - 1)) == 0, "sorting fills a list up to a power of two");
 static_assert(kList >= 2 * SDMS_MAX_BEAM_PATHS && kRowList >= SDMS_MAX_BEAM_PATHS, "the N best and another list's");
+static_assert((SDMS_MAX_BEAM_PATHS & (SDMS_MAX_BEAM_PATHS - 1)) == 0 && SDMS_MAX_BEAM_PATHS <= kRowThreads, "a group is a thread at least");
 constexpr int kMergeThreads = 512;
 constexpr int kRanked = 384;              // candidates up to which ranks are counted instead of sorting (1024: 1 x 128 rows of 151936 183 for 126 us)
 constexpr int kKnownFrom = 4 * 148 * 4;
@@ -276,7 +277,7 @@ beam_rows_kernel(int paths, int vocab, int chunks, int rows, const T* logits, in
   // groups of threads: the smallest power of two from N, 16 at least
   int groups = 16;
   while (groups < paths) groups <<= 1;
-  const int lanes = kRowThreads / groups;                           // 32 .. 2
+  const int lanes = kRowThreads / groups;                           // 16 .. 1
   float most, least;
   double total;
   for (int pass = 0;; ++pass) {
