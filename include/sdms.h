@@ -422,7 +422,7 @@ typedef struct {
 /*
  * Row r of the cache takes d_k_new / d_v_new [rows][tokens][heads][head_dim] (contiguous, 16-byte aligned) at token
  * positions d_len[r] + t, t < d_count[r] (NULL: all `tokens`).  Types: the cache's own, BF16 for E4M3 caches.  Positions that the
- * cache does not have are left out; a count above `tokens` counts as `tokens`, a negative count or length as 0.  The lengths are the caller's to
+ * cache does not have are left out; a count above `tokens` (1 or more) counts as `tokens`, a negative count or length as 0.  The lengths are the caller's to
  * raise: a draft that is refused costs nothing, the next call writes over it.
  * E4M3: the scale of a token and head is the smallest power of two 2^b, b >= -127, with |x| <= 448 * 2^b for all of its
  * elements; x / 2^b is rounded to the nearest of the 8-bit values, ties to even.  A vector with an infinity or NaN is stored as
@@ -448,7 +448,7 @@ int sdms_kv_reorder(const sdms_kv* kv, const int32_t* d_parent, const int32_t* d
  * T = 1 is plain decoding, T = D + 1 the check of a draft.
  * `prefix` or `paths` may be NULL, with its lengths.  Lengths are clamped to [0, capacity], counts to [0, T].  A query that sees
  * nothing gives 0; queries t >= d_count[p] leave d_out as it is.  An infinity or NaN in V of a
- * new token makes all elements of the queries that see it NaN (with T = 1 and no mask: those elements what they are) and touches no
+ * new token makes all elements of the queries that see it NaN (of a path with one query and without a mask: those elements what they are) and touches no
  * other query; what lies behind the lengths may be anything.
  * Types: q, out and caches all BF16 or all FP16, or BF16 with E4M3 caches.  The products' sums, softmax and its statistics are
  * held in 32 bits; weights are rounded to the query's type for the second product (FP16: what is below 2^-31 of the largest counts as nothing there).
@@ -468,7 +468,7 @@ typedef struct {
   int32_t  dtype;              /* of q and out: SDMS_TYPE_BF16 or _FP16    */
   int64_t  q_stride_path, q_stride_token, q_stride_head;      /* in elements */
   int64_t  out_stride_path, out_stride_token, out_stride_head;
-  float    scale;              /* positive and finite                      */
+  float    scale;              /* positive, below 1e30                     */
   int32_t  reserved;           /* must be 0                                */
 } sdms_attention;
 
@@ -483,7 +483,9 @@ int sdms_attend(const sdms_attention* cfg, const sdms_kv* prefix, const int32_t*
  * Beam search's selection.  Path p of score d_scores[p] and logits x = d_logits[p * row_stride + 0 .. vocab) offers a
  * candidate per token v, worth d_scores[p] + x_v - log(sum_w exp x_w); a path with d_done[p] != 0 (d_done may be NULL) offers itself once,
  * at its score, with token done_token.  The paths_per_group best candidates of a prompt become its paths, ties going to the lowest path
- * and in it to the lowest token (to the larger logit, where only the sum makes them equal).  Worth is compared in 64 bits and rounded once, to d_score.  A logit of -infinity or NaN is a token that is not there, +infinity
+ * and in it to the lowest token (to the larger logit, where only the sum makes them equal).  Worth is added up and compared in
+ * 64 bits and rounded once, to d_score; the sum's terms are exponentials of 32 bits, so worths of different paths that lie within 2^-20 of each other may
+ * come in either order (those of one path, and of paths whose scores and logits are the same, never do).  A logit of -infinity or NaN is a token that is not there, +infinity
  * counts as the type's largest value, a path whose score is -infinity or NaN (or all of whose logits are not there) offers nothing.
  * The best child of a path takes its parent's place, the others the places left over, best first: d_parent[p] (a path
  * index) is what sdms_reorder and sdms_kv_reorder take, and only paths with d_parent[p] != p have to be copied.  Places
