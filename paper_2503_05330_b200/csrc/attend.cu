@@ -13,10 +13,14 @@
 // than 128 rows has a sum for each half of them, both over the same tiles of K and V.  Warp 8 fetches tiles (TMA), warp 9 asks for the products, warp
 // 10 (8-bit caches: 10-17, which turn 8 bits into 16) sees to what lies behind the last key, one more deals the segments.
 //
-// What bounds it (head 128): 64 x 5 tokens behind 65536 keys, 380 us: the softmax warps, 2100 cycles a tile of which 1160 are exponentials, the products
-// 1026 (910 TFLOP/s; the power limit shows); 16 x 1 behind 32768, 46 us: K and V of a tile in 2500 cycles, which is the memory's rate, and 15 us in front
-// of the first tile and behind the last; 32 x 16 x 1 in 16 bits, 225 us: 5.4 TB/s; 16 x 9 with 8-bit caches, 71 us: the conversion and the steps of few
-// rows; the smallest, 10 us: its chain of lengths, segment, Q and K, products, join.
+// Weights are rounded to the query's 16 bits for the second product, which takes no others; their total is not.  Outputs are 0.0019 to 0.0023 from 64 bits (rms,
+// relative) in bfloat16 and 0.00029 in fp16, where rounding the output alone leaves 0.0017 and 0.00021.
+//
+// What bounds it (head 128; back to back, and called one by one where that differs): 64 x 5 tokens behind 65536 keys, 370 to 425 us (927 to 805 TFLOP/s, by the power
+// limit): the chain of one tile, 2100 cycles in the softmax warps of which 1160 are exponentials; the products' 1026 hide behind it.  16 x 1 behind 32768, 46 us: K and V
+// of a tile in 2500 cycles, which is the memory's rate, and 15 us in front of the first tile and behind the last.  32 x 16 x 1 in 16 bits, 216 us (5.6 TB/s), 247 one
+// by one.  8-bit caches, the conversion and the steps of few rows: 16 x 9, 76 us; 32 x 16 x 1, 381.  The smallest, 10.5 us: its chain of lengths, segment, Q and K,
+// products, join.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

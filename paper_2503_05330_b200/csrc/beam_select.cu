@@ -14,9 +14,10 @@
 // Where a row's chunks do not all run at once, later ones know how good the N best of an earlier one are (a word a row, which only goes up): what lies
 // below is not listed.  Which chunk knew of which changes what is listed, never what is selected.
 //
-// What bounds it: 32 x 16 rows of 151936 in 16 bits take 96 us, of which the bytes are 21: issue slots (69 % used), 50 for the maximum and the bound, 20
-// for the sums, the rest for listing and sorting (39 where no chunk knows of another: 108 us).  1 x 16 of 128256: 14.3, 1 x 4 of 32000: 8.2, the two launches' chain of latencies.
-// Prompts of many paths, the merge's one CTA and the rows' lists: 1 x 256 of 32000 232 us, of 151936 303; 1 x 64 of 128256 74.
+// What bounds it: 32 x 16 rows of 151936 in 16 bits take 96 us, of which the bytes are 21.  Neither the memory (16 % busy) nor the issue slots (69 % used) are
+// full: a CTA waits for its chunk, and the loads overlap with the three other CTAs of its SM only.  By leaving parts out: loads, maximum and bound 50, sums 20, the
+// rest listing and sorting (39 where no chunk knows of another: 108 us).  1 x 16 of 128256: 14 to 15, 1 x 4 of 32000: 8.1 in a graph, 11 by a call, the two launches'
+// chain of latencies.  Prompts of many paths, the merge's one CTA and the rows' lists: 1 x 256 of 32000 222 us, of 151936 303; 1 x 64 of 128256 77.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>

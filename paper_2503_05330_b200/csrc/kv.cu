@@ -2,9 +2,12 @@
 //
 // sdms_kv_append   scale of a token and head: the smallest power of two 2^b with max |x| <= 448 * 2^b.  A power of two loses
 //                  nothing that 8 bits with an exponent would keep (x / 2^b has x's own mantissa), costs one byte, and makes what attention
-//                  reads back, code * 2^b, exact in bfloat16: the products see it without a second rounding.
-//                  Bounded by bytes in flight: 32 x 4096 tokens of 8 heads of 128, 168 us, 4.85 TB/s; 512 x 9: 7.7, a launch's latency.
-// sdms_kv_reorder  copies of rows, bounded by bytes: 276 us for 2.0 GB read and written (what was read twice comes from the L2), 7.8 for 16 rows of 1024.
+//                  reads back, code * 2^b, exact in bfloat16: the products see it without a second rounding.  (But for 256 * 2^120, which numbers
+//                  next to the largest bfloat16 round to.)
+//                  32 x 4096 tokens of 8 heads of 128: 16 bits 163 us, 6.6 TB/s, the memory's rate; 8 bits 167 us, 4.85 TB/s, bounded by instructions (74 %
+//                  of issue slots, DRAM 44 %).  512 x 9: 6.2 and 7.7 us, a launch and four to five waves of CTAs of one item a thread.
+// sdms_kv_reorder  copies of rows, bounded by bytes: 278 to 296 us for 2.0 GB read and written (what was read twice comes from the L2), 7.6 for 16 rows of
+//                  1024 (8.5 called one by one).
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include "decode_internal.h"
