@@ -107,3 +107,27 @@ def test_codes_that_are_not_numbers_behind_the_last_key():
             x.view(torch.uint8)[:, 100:] = 0xff
     out, expect, tol = spoiled_attention(128, 3, [1, 130, 257], 100, spoil)
     assert bool(torch.isfinite(expect).all()) and bool(((out.double() - expect).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("scale", [121, 140])
+def test_codes_that_are_not_numbers_wherever_a_tile_has_them(d, scale):
+    """A path for every token of a tile, its code at another element each time: all tokens, elements and places of a word come up."""
+    P = 2 * 128
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(d + scale)
+    paths = make_cache(P, 256, 1, d, torch.float8_e4m3fn, gen)
+    p = torch.arange(P, device=DEV)
+    token, element = p % 128 + 128 * (p % 2), (p * 5 + p // 128 * 3) % d
+    assert len(set((token % 128).tolist())) == 128 and len(set(element.tolist())) == d
+    paths.v.view(torch.uint8)[p, token, 0, element] = torch.where(p % 3 == 0, 0xff, 0x7f).to(torch.uint8)
+    paths.v_scale[p, 0, token] = scale
+    q = torch.randn((P, 1, 2, d), device=DEV, generator=gen).to(torch.bfloat16)
+    out = torch.full_like(q, 7.0)
+    lens = torch.full((P,), 255, device=DEV, dtype=torch.int32)
+    binding.PathAttention(1, P, 1, 2, 1, d, torch.bfloat16)(q, out, paths, lens)
+    expect, tol = ref.attend(q, ref.cache_values(paths.k, paths.k_scale), ref.cache_values(paths.v, paths.v_scale), [255] * P, None, d ** -0.5)
+    want = torch.isnan(expect)
+    assert int(want.sum()) == 2 * P
+    assert torch.equal(torch.isnan(out), want)
+    assert bool(((out.double() - expect).abs() <= tol)[~want].all())
